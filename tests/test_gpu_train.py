@@ -675,6 +675,31 @@ def test_adamw_many_small_and_one_large_tensor(bits):
     assert all(torch.equal(a, b) for a, b in zip(p, q))
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("lr,wd", [(1e-5, 0.05), (2.5e-6, 0.01)])
+def test_adamw_small_decays_add_up(bits, lr, wd):
+    """Two runs of 400 steps on the same gradients, one with decay: without rounding,
+    their parameters part by lr wd times the sum of the decayed run's parameters.
+    A step rounds a parameter of 0.5 to 1 by 2^-25 at most, at random: the updates
+    of the two runs are of 40 to 170 units in the last place and new at every step.  Over
+    400 steps and 65536 entries the mean of the two walks is within 6 sqrt(2) 2^-25
+    sqrt(400 / (3 * 65536)) = 1.2e-8; the decays are 1.5e-4 and 7.5e-6 in all."""
+    torch, dev = torch_dev()
+    n, steps = 1 << 16, 400
+    gen = torch.Generator(device=dev).manual_seed(1)
+    start = 0.5 + 0.5 * torch.rand(n, device=dev, generator=gen)
+    p, g = [start.clone(), start.clone()], torch.zeros(n, device=dev)
+    sets = [T.TensorSet([q], [g], state_bits=bits, weight_decay=d) for q, d in zip(p, (wd, 0.0))]
+    total = torch.zeros((), dtype=torch.float64, device=dev)
+    for step in range(1, steps + 1):
+        g.normal_(generator=gen)
+        total += p[0].double().mean()
+        for s in sets:
+            T.adamw_step(s, step, lr, seed=2)
+    parted = (p[1].double() - p[0].double()).mean().item()
+    assert abs(parted - lr * wd * total.item()) <= 5e-8
+
+
 def test_sets_refuse_on_the_device():
     torch, dev = torch_dev()
     p, g = torch.zeros(10, device=dev), torch.zeros(10, device=dev)
