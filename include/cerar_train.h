@@ -106,11 +106,12 @@ int cerar_adamw_pack(const cerar_adamw *hyper, cerar_adamw_values *values);
  *   g = grad * (grad_scale * clip[1]);  m = beta1 m + (1 - beta1) g;
  *   v = beta2 v + (1 - beta2) g^2;
  *   param = param (1 - lr' wd) - lr' / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * with lr' = lr * lr_scale.  m and v are formed in fp64 and rounded to fp32
- * once a step (the averages of thousands of steps, whose terms cancel), the
- * rest is fp32; param is rounded once to its type.  The step uses m and v
- * before they are rounded to 8 bits.  That rounding is
- * stochastic: in blocks of 128 entries, whose scale is the smallest power of
+ * with lr' = lr * lr_scale.  m and v are formed in fp64 (the averages of thousands
+ * of steps, whose terms cancel), the rest is fp32; param is rounded once to its
+ * type.  32-bit states are rounded to nearest once a step.  With 8-bit states the
+ * step uses m and v cut off to fp32's 24 bits, before they are rounded to 8; a v
+ * beyond fp32's range is infinite with either width, and its param then takes the decay
+ * alone.  The rounding to 8 bits is stochastic: in blocks of 128 entries, whose scale is the smallest power of
  * two that holds the largest, |x| is rounded up with the probability that its
  * remainder has (16 random bits from a hash of seed, step and the entry's
  * place in the set), so that an average that moves by less than a code's

@@ -158,7 +158,8 @@ __device__ inline uint32_t any_code(float a, uint32_t r) {
     const bool small = a < C::kLow;
     const uint32_t t = __float_as_uint(small ? a + C::kLow : a) - ((small ? C::kFields + 1 : C::kFields) << 23);
     uint32_t code = (t + (r << (C::kDrop - 16))) >> C::kDrop;
-    return __builtin_isfpclass(a, 0x207) ? 0x7Fu : code;         // NaN, infinite
+    if (F == CERAR_E5M2) code = __builtin_isfpclass(a, 0x200) ? 0x7Cu : code;    // infinite, where the format has it
+    return __builtin_isfpclass(a, F == CERAR_E5M2 ? 0x3 : 0x203) ? 0x7Fu : code;   // NaN
 }
 
 // A lane's states, magnitudes in a (fp32 bits) and signs in the top bits of
@@ -208,12 +209,11 @@ __device__ inline void store_codes(uint8_t *codes, uint8_t *scale, int left, con
 
 // Magnitude of an fp64 value as fp32 bits, cut off: what goes lies below the last of
 // the 16 places that a code's rounding compares, so the code is that of the fp64
-// value.  Beyond fp32's range: below 2^-127 a number of that size or less, 0 for 0,
-// and infinity or NaN above.
+// value.  The conversion rounds subnormal numbers only; from 2^128 on it gives infinity,
+// as rounding does for 32-bit states.
 __device__ inline uint32_t cut_off(double x) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t hi = min(max((uint32_t)(u >> 32) & 0x7FFFFFFFu, 0x38000000u), 0x47F00000u);
-    return __builtin_amdgcn_alignbit(hi, (uint32_t)u, 29) - 0xC0000000u;
+    const uint64_t u = __builtin_bit_cast(uint64_t, x) & 0x7FFFFFFFE0000000ull;
+    return __float_as_uint((float)__builtin_bit_cast(double, u));
 }
 
 // A workgroup's sweep.  The averages are formed in fp64 and rounded once.  sqrt and

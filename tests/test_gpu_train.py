@@ -636,6 +636,48 @@ def test_adamw_8_bit_squares_far_below_their_block_stay_above_zero():
     assert codes[1] == 1 and codes[2] == 1 and codes[0] >= 0x78 and not codes[3:].any()
 
 
+def test_adamw_8_bit_squares_beyond_fp32_are_infinite_as_32_bit_ones_are():
+    """Finite gradients whose square passes 2^128: the second average is infinite and the
+    step zero, for 8-bit states as for 32-bit ones, at this step and at later ones."""
+    torch, dev = torch_dev()
+    n, huge = 300, {3: 1e21, 5: -1e21, 130: 1.7e22, 131: 1e25, 260: -1e30, 299: 3e38}
+    p, g = [], torch.full((n,), 1e-2, device=dev)
+    for i, x in huge.items():
+        g[i] = x
+    at, rest = list(huge), [i for i in range(n) if i not in huge]
+    for bits in (32, 8):
+        q = torch.linspace(1.0, 2.0, n, device=dev)
+        start = q.clone()
+        s = T.TensorSet([q], [g], state_bits=bits)
+        for step in range(1, 4):
+            T.adamw_step(s, step, 1e-3, seed=step)
+            assert torch.equal(q[at], start[at]) and bool(torch.isfinite(q).all())
+            if step == 1:
+                p.append(q[rest].clone())
+        m, v = s.states["m"][0].double(), s.states["v"][0].double()
+        assert bool(torch.isfinite(m).all()) and bool(torch.isinf(v[at]).all()) and bool(torch.isfinite(v[rest]).all())
+    # the first step is of 1e-3 from exact states of zero: fp32's 24 bits against 24 bits cut off, then the parameter's rounding
+    assert (p[0] - p[1]).abs().max().item() <= 8 * U32 * 1e-3 + 2 * U32 * 2
+
+
+def test_adamw_8_bit_states_below_the_normal_numbers():
+    """Averages of 2^-136 to 2^-122, in blocks whose scale is the smallest: the oracle's
+    codes.  fp32 holds a number of 2^-136 to 2^-14 of it, a code's spacing is an eighth or
+    more of a number: of the 1024 entries one or two may fall on the neighbour."""
+    torch, dev = torch_dev()
+    rng = np.random.default_rng(21)
+    for name, fmt, g in (("v", "e5m2", 2.0 ** rng.uniform(-68, -61, 1024)), ("m", "e4m3", 2.0 ** rng.uniform(-125, -119, 1024))):
+        t, g = device(g)
+        s = T.TensorSet([torch.zeros(1024, device=dev)], [t], state_bits=8)
+        # beta2 = 0 and beta1 = 0.875: v = g^2 and m = g / 8, exact in fp64
+        T.adamw_step(s, 1, 1e-3, beta1=0.875, beta2=0.0, seed=5)
+        r = dict(zip("mv", O.chances(1024, 0, 5, 1)))[name]
+        codes, k = O.round_by_chance(g * g if name == "v" else g / 8, fmt, r)
+        np.testing.assert_array_equal(host8(s.states[name + "_scale"][0]), k + 127)
+        diff = host8(s.states[name][0]).astype(int) - codes
+        assert (np.abs(diff) <= 1).all() and (diff != 0).sum() <= 2, (name, (diff != 0).sum())
+
+
 def test_norm_beyond_fp32_is_infinite_and_nothing_is_stepped():
     torch, dev = torch_dev()
     g = torch.full((5000,), 3e38, device=dev)
