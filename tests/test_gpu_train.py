@@ -779,6 +779,68 @@ def test_sets_refuse_on_the_device():
         T.matmul_blocks(w, T.Blocks.empty(6, 301), torch.zeros((6, 6), device=dev))
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_backward_that_saved_what_a_step_wrote_raises(bits):
+    """Parameters and their copies count the step's writes, whether they are tensors of
+    their own or views of one; a step that is refused counts nothing."""
+    torch, dev = torch_dev()
+    flat = torch.ones(600, device=dev)
+    p = [torch.nn.Parameter(torch.ones(200, device=dev)), flat[:300].view(20, 15), flat[300:]]
+    g = [torch.full_like(t, 1e-2) for t in p]
+    cp = [torch.zeros_like(t, dtype=torch.bfloat16) for t in p]
+    s = T.TensorSet([t.detach() if t.requires_grad else t for t in p], g, state_bits=bits, copies=cp)
+    x = torch.ones((), device=dev, requires_grad=True)
+
+    def losses():
+        return [t.square().sum() if t.requires_grad else (x * t).sum() for t in p + cp]
+
+    for loss in losses():
+        loss.backward()                                  # none has been written since
+    saved = losses()
+    with pytest.raises(C.CerarError):
+        T.adamw_step(s, 0, 1e-3)
+    saved.pop(0).backward()
+    saved = losses()
+    T.adamw_step(s, 1, 1e-3)
+    for loss in saved:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    for loss in losses():
+        loss.backward()
+    T.adamw_step(s, values=T.adamw_values(2, 1e-3).to(dev))
+    assert [t._version for t in s._stepped] == [2] * len(s._stepped)
+
+
+def test_a_backward_that_saved_a_product_raises_once_it_is_overwritten():
+    torch, dev = torch_dev()
+    a, w = T.Blocks.empty(5, 300), T.Blocks.empty(6, 300)
+    v = torch.ones((5, 300), device=dev)
+    T.quantize_blocks(v, rows=a)
+    T.quantize_blocks(torch.ones((6, 300), device=dev), rows=w)
+    x, out = torch.ones((), device=dev, requires_grad=True), torch.zeros((5, 6), device=dev)
+    for call in (lambda: T.matmul_blocks(a, w, out), lambda: T.matmul_blocks(a, w, out, accumulate=True),
+                 lambda: T.linear_blocks(v, w, out, workspace(5, 6, 300, True))):
+        (x * out).sum().backward()
+        loss = (x * out).sum()
+        call()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+
+
+def test_inference_tensors_are_stepped_and_written():
+    torch, dev = torch_dev()
+    with torch.inference_mode():
+        p, g = torch.ones(10, device=dev), torch.ones(10, device=dev)
+        s = T.TensorSet([p[:4], p[4:]], [g[:4], g[4:]])
+        T.adamw_step(s, 1, 1e-3)
+        assert bool((p < 1).all())
+        w = T.Blocks.empty(6, 300)
+        T.quantize_blocks(torch.ones((6, 300), device=dev), rows=w)
+        out = torch.zeros((1, 6), device=dev)
+        T.linear_blocks(torch.ones((1, 300), device=dev), w, out, workspace(1, 6, 300, True))
+        assert bool((out == 300).all())
+
+
 # --- streams and graphs --------------------------------------------------------------------
 
 class Problem:
