@@ -212,6 +212,59 @@ def group_bound(A, B):
     return 8 * 2.0 ** -12 * worst + sum_bound(A, B)
 
 
+SUMS = [(1, 500, 4096), (40, 300, 2048), (64, 130, 2048), (70, 200, 1024), (129, 257, 640), (130, 120, 16384), (4352, 4480, 256),
+        (4200, 4300, 384), (203, 12108, 10240), (3000, 3000, 16384)]
+
+
+@pytest.mark.parametrize("M,N,K", SUMS)
+@pytest.mark.parametrize("name,add", [("f32", False), ("f32", True), ("bf16", False)])
+def test_fp32_sums_keep_a_term_far_below_its_neighbours(M, N, K, name, add):
+    """Eight neighbouring terms are 1, -1, 2^-16 and zeros.  Groups of them add up to K 2^-19 without a
+    rounding in fp32 (multiples of 2^-16 below 2^8); the 8-bit instruction loses the small terms.  K is a
+    power of two times 5 at most, so that bf16 holds the result.  Tiles of either size, whole K and K in
+    parts, whole tiles and their edges, and few rows."""
+    torch, dev = torch_dev()
+    codes = torch.zeros((1, K), dtype=torch.uint8, device=dev)
+    codes[:, 0::8], codes[:, 3::8], codes[:, 6::8] = 0x38, 0x38, 0x02        # 1, 1, 2^-8
+    signed = codes.clone()
+    signed[:, 3::8] = 0xB8                                                   # -1
+
+    def operand(codes, rows, seed):
+        gen = torch.Generator(device=dev).manual_seed(seed)
+        k = torch.randint(-3, 4, (rows,), device=dev, generator=gen)
+        scales = torch.zeros((-(-K // 512), rows, 4), dtype=torch.uint8, device=dev)
+        for b in range(K // 128):
+            scales[b // 4, :, b % 4] = (k + 127).to(torch.uint8)
+        return T.Blocks(codes.expand(rows, K).contiguous().view(torch.float8_e4m3fn), scales, K), 2.0 ** k.double()
+
+    (a, fa), (b, fb) = operand(codes, M, 1), operand(signed, N, 2)
+    want = fa[:, None] * fb[None, :] * (K / 2.0 ** 19)
+    out, _ = out_buffer(M, N, name)
+    out.zero_()
+    T.matmul_blocks(a, b, out, workspace(M, N, K), accumulate=add)
+    assert torch.equal(out.double(), want)
+    if M > 64 and not add and name == "f32":
+        T.matmul_blocks(a, b, out, workspace(M, N, K), fast_sums=True)
+        assert not bool((out.double() == want).any())
+
+
+@pytest.mark.parametrize("M,N,K", [(30, 70, 8192), (100, 90, 1000), (130, 120, 16000), (700, 530, 9000), (1030, 270, 2049),
+                                   (3000, 3000, 16384)])
+def test_fp32_sums_of_long_rows_are_those_of_fp32(M, N, K):
+    """Each of K additions rounds by 2^-24 of a partial sum at most, which is no larger than the
+    result in the mean over results: 2^-24 sqrt(K) of it in all, if the roundings are
+    independent, where the 8-bit instruction is off by 1.5e-5 to 5e-5 whatever K."""
+    torch, dev = torch_dev()
+    rng = np.random.default_rng(K)
+    a, b = random_blocks(rng, M, K, "e5m2", 126, 129), random_blocks(rng, N, K, "e4m3", 126, 129)
+    out, _ = out_buffer(M, N, "f32")
+    T.matmul_blocks(a, b, out, workspace(M, N, K))
+    rows = np.unique(rng.integers(0, M, 150))
+    ref = values(a)[rows] @ values(b).T
+    err = out.double().cpu().numpy()[rows] - ref
+    assert math.sqrt((err ** 2).mean()) <= U32 * math.sqrt(K) * math.sqrt((ref ** 2).mean())
+
+
 @pytest.mark.parametrize("M,N,K", SHAPES)
 @pytest.mark.parametrize("fa,fb", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e5m2")])
 def test_fast_sums_match_oracle(M, N, K, fa, fb):
