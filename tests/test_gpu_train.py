@@ -313,6 +313,92 @@ def test_large_matmul_matches_oracle(M, N, K, fast, name, add):
     assert bool((buf[:1] == 7).all()) and bool((whole[:, N:] == 7).all()) and bool((buf[1 + M * (N + 3):] == 7).all())
 
 
+def bound_of_few(A, B, fast):
+    """group_bound or sum_bound where A or B has few rows, one of them at a time."""
+    if B.shape[0] < A.shape[0]:
+        return bound_of_few(B, A, fast).T
+    B = np.abs(B)
+    tol = np.zeros((A.shape[0], B.shape[0]))
+    for i, a in enumerate(np.abs(A)):
+        tol[i] = A.shape[1] * 2.0 ** -23 * (B @ a)
+        if fast:
+            tol[i] += 8 * 2.0 ** -12 * np.maximum.reduceat(B * a, np.arange(0, len(a), 8), axis=1).sum(1)
+    return tol
+
+
+@pytest.mark.parametrize("M,N,K,pad,fast", [
+    (4352, 4480, 300, 0, True), (4352, 4480, 300, 0, False),         # 256 x 256: rows on cache lines, whole and edge columns
+    (4400, 4300, 130, 52, True), (4400, 4300, 130, 52, False),       # and with a padded row, edges both ways
+    (4400, 4300, 100, 0, True), (4400, 4352, 128, 0, True),          # one block of K
+    (5345, 1075, 12235, 1, True), (203, 12108, 9999, 4, False), (203, 12108, 9999, 0, True),   # 256 x 256 with K in parts
+    (640, 768, 700, 0, True), (640, 768, 700, 0, False), (700, 650, 515, 118, True)])          # 128 x 128 on cache lines
+@pytest.mark.parametrize("name,add", [("bf16", False), ("f32", False), ("f32", True)])
+def test_every_way_that_tiles_leave_matches_oracle(M, N, K, pad, fast, name, add):
+    """Whole tiles and edges, stored past the L2 and through it, from either size of tile, and joined."""
+    rng = np.random.default_rng(M + N + K)
+    a, b = random_blocks(rng, M, K, "e5m2" if add else "e4m3"), random_blocks(rng, N, K, "e4m3")
+    start = rng.standard_normal((M, N)).astype(np.float32) * 1e4 if add else None
+    out, buf = out_buffer(M, N, name, pad=pad, fill=start)
+    T.matmul_blocks(a, b, out, workspace(M, N, K), accumulate=add, fast_sums=fast)
+    A, B, got = values(a), values(b), out.double().cpu().numpy()
+    count = 40 if K < 1000 else 3
+    for rows, cols in ((np.unique(rng.integers(0, M, count)), np.arange(N)), (np.arange(M), np.unique(rng.integers(0, N, count)))):
+        ref = A[rows] @ B[cols].T + (start[np.ix_(rows, cols)].astype(np.float64) if add else 0.0)
+        tol = bound_of_few(A[rows], B[cols], fast) + 4 * U32 * np.abs(ref)
+        if add:
+            tol = tol + 2 * U32 * np.abs(start[np.ix_(rows, cols)])
+        if name == "bf16":
+            tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref)
+        assert (np.abs(got[np.ix_(rows, cols)] - ref) <= tol).all()
+    assert bool((buf[:M * (N + pad)].view(M, N + pad)[:, N:] == 7).all()) and bool((buf[M * (N + pad):] == 7).all())
+
+
+@pytest.mark.parametrize("M,N", [(100, 70), (300, 300), (4400, 4352)])
+@pytest.mark.parametrize("fast", [False, True])
+def test_more_rows_of_no_columns(M, N, fast):
+    torch, dev = torch_dev()
+    a, b = T.Blocks.empty(M, 0), T.Blocks.empty(N, 0)
+    for name in ("f32", "bf16"):
+        out, _ = out_buffer(M, N, name, pad=1)
+        if name == "f32":
+            T.matmul_blocks(a, b, out, workspace(M, N, 0), accumulate=True, fast_sums=fast)
+            assert bool((out == 7).all())
+        T.matmul_blocks(a, b, out, workspace(M, N, 0), fast_sums=fast)
+        assert bool((out == 0).all())
+        out.fill_(7)
+        T.linear_blocks(torch.empty((M, 0), device=dev), b, out, workspace(M, N, 0, True), fast_sums=fast)
+        assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("lo,hi", [(1, 3), (240, 248)])
+@pytest.mark.parametrize("M,N,K", [(30, 90, 400), (70, 90, 400), (300, 270, 700)])
+def test_fast_sums_of_scales_at_both_ends(M, N, K, lo, hi):
+    rng = np.random.default_rng(4)
+    a, b = random_blocks(rng, M, K, "e4m3", lo, hi), random_blocks(rng, N, K, "e4m3", 254 - hi, 254 - lo)
+    out, _ = out_buffer(M, N, "f32")
+    T.matmul_blocks(a, b, out, workspace(M, N, K), fast_sums=True)
+    A, B = values(a), values(b)
+    ref = A @ B.T
+    assert (np.abs(out.double().cpu().numpy() - ref) <= group_bound(A, B) + 2 * U32 * np.abs(ref)).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(4352, 4480, 300), (203, 12108, 9999), (8192, 4096, 2048)])
+def test_large_products_repeat_their_bits(M, N, K):
+    """Also after calls on other operands, whose codes the chip's caches then hold."""
+    torch, dev = torch_dev()
+    rng = np.random.default_rng(8)
+    a, b = random_blocks(rng, M, K, "e4m3"), random_blocks(rng, N, K, "e4m3")
+    other = random_blocks(rng, M, K, "e4m3")
+    ws, out, scratch = workspace(M, N, K), out_buffer(M, N, "bf16")[0], out_buffer(M, N, "bf16")[0]
+    first = {}
+    for k in range(8):
+        fast = k % 2 == 1
+        T.matmul_blocks(other, b, scratch, ws, fast_sums=fast)
+        out.fill_(7)
+        T.matmul_blocks(a, b, out, ws, fast_sums=fast)
+        assert torch.equal(first.setdefault(fast, out.clone()), out)
+
+
 def test_matmul_applies_each_scale_to_its_block():
     """One code of one in each operand's row and column: entry (m, n) is the sum
     over blocks of 2^(ka + kb), exact in fp32, whatever the scales' layout."""
