@@ -6,7 +6,8 @@
  * The conventions of cerar.h hold (statuses, cerar_last_error, device
  * pointers owned by the caller, calls that only validate and enqueue kernel
  * launches on the stream that they are given, so that they can be recorded
- * into a HIP graph).
+ * into a HIP graph).  Row strides (ld) are in entries; one that takes a matrix
+ * of more than a row past 2^56 bytes is refused.
  *
  * Block format.  A matrix (rows x cols) in 8-bit floating point: `codes`
  * holds rows of ld = cols rounded up to a multiple of 128 bytes, zeros beyond

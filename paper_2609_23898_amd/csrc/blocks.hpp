@@ -27,6 +27,17 @@ inline bool ranges_meet(const void *a, size_t na, const void *b, size_t nb) {
     return na && nb && x < y + nb && y < x + na;
 }
 
+// Bytes from the first entry of a matrix to its last, or false where they pass 2^56, more
+// than any address space.
+inline bool matrix_bytes(size_t rows, size_t cols, size_t ld, size_t entry, size_t *bytes) {
+    constexpr size_t most = (size_t)1 << 56;
+    *bytes = 0;
+    if (!rows || !cols) return true;
+    if (cols > most / entry || (rows > 1 && ld > (most / entry - cols) / (rows - 1))) return false;
+    *bytes = ((rows - 1) * ld + cols) * entry;
+    return true;
+}
+
 namespace {
 
 // Exponent of the largest binade: its largest value is 1.75 * 2^kTop.

@@ -607,6 +607,8 @@ int check_product(size_t M, size_t N, const cerar_blocks *b, void *out, cerar_ty
     if ((unsigned)sums > CERAR_SUMS_FAST) return fail(CERAR_E_INVAL, "unknown sums");
     if (M >= (size_t)1 << 31) return fail(CERAR_E_INVAL, "a size of 2^31 or more");
     const size_t entry = out_type == CERAR_F32 ? 4 : 2;
+    size_t bytes;
+    if (!matrix_bytes(M, N, ld_out, entry, &bytes)) return fail(CERAR_E_INVAL, "ld_out=%zu passes the address space", ld_out);
     if (M && N) {
         if (!out) return fail(CERAR_E_INVAL, "NULL out");
         if (ld_out < N) return fail(CERAR_E_INVAL, "ld_out=%zu below N=%zu", ld_out, N);
@@ -616,7 +618,7 @@ int check_product(size_t M, size_t N, const cerar_blocks *b, void *out, cerar_ty
     }
     spans[used++] = {b->codes, b->rows * blocks_ld(b->cols), "b"};
     spans[used++] = {b->scales, b->rows * scale_groups(b->cols) * 4, "b"};
-    const Span written[2] = {{out, M && N ? ((M - 1) * ld_out + N) * entry : 0, "out"}, {ws, ws_bytes, "ws"}};
+    const Span written[2] = {{out, bytes, "out"}, {ws, ws_bytes, "ws"}};
     for (const Span &w : written)
         for (int i = 0; i < used; ++i)
             if (ranges_meet(w.p, w.n, spans[i].p, spans[i].n)) return fail(CERAR_E_INVAL, "%s and %s overlap", w.name, spans[i].name);
@@ -669,11 +671,13 @@ extern "C" int cerar_linear_blocks(const void *x, cerar_type type, size_t M, siz
     const size_t K = w->cols, entry = type == CERAR_F32 ? 4 : 2;
     if ((unsigned)type > CERAR_BF16) return fail(CERAR_E_INVAL, "unknown type");
     if (ld < K) return fail(CERAR_E_INVAL, "ld=%zu below cols=%zu", ld, K);
-    if (M && K && !x) return fail(CERAR_E_INVAL, "NULL x");
+    size_t x_bytes;
+    if (!matrix_bytes(M, K, ld, entry, &x_bytes)) return fail(CERAR_E_INVAL, "ld=%zu passes the address space", ld);
+    if (x_bytes && !x) return fail(CERAR_E_INVAL, "NULL x");
     if (reinterpret_cast<uintptr_t>(x) % entry) return fail(CERAR_E_INVAL, "x is not aligned to its entries");
     size_t ws_bytes = 0;
     if ((st = cerar_matmul_workspace_bytes(M, w->rows, K, 1, &ws_bytes)) != CERAR_OK) return st;
-    Span spans[6] = {{x, M && K ? ((M - 1) * ld + K) * entry : 0, "x"}};
+    Span spans[6] = {{x, x_bytes, "x"}};
     st = check_product(M, w->rows, w, out, out_type, ld_out, sums, ws, ws_bytes, spans, 1);
     if (st != CERAR_OK || M == 0 || w->rows == 0) return st;
     const hipStream_t hs = reinterpret_cast<hipStream_t>(stream);

@@ -254,7 +254,8 @@ extern "C" int cerar_quantize_blocks(const void *x, cerar_type type, size_t rows
     if (rows >= (size_t)1 << 31 || cols >= (size_t)1 << 31) return fail(CERAR_E_INVAL, "x has a size of 2^31 or more");
     if (ld < cols) return fail(CERAR_E_INVAL, "ld=%zu below cols=%zu", ld, cols);
     const size_t entry = type == CERAR_F32 ? 4 : 2;
-    const size_t bytes = rows && cols ? ((rows - 1) * ld + cols) * entry : 0;
+    size_t bytes;
+    if (!matrix_bytes(rows, cols, ld, entry, &bytes)) return fail(CERAR_E_INVAL, "ld=%zu passes the address space", ld);
     if (bytes && !x) return fail(CERAR_E_INVAL, "NULL x");
     if (reinterpret_cast<uintptr_t>(x) % entry) return fail(CERAR_E_INVAL, "x is not aligned to its entries");
     struct Span {

@@ -202,6 +202,19 @@ def test_more_work_than_a_launch_takes_is_refused():
     assert b"too large" in T.lib().cerar_last_error()
 
 
+@pytest.mark.parametrize("ld", [1 << 54, 1 << 61, (1 << 62) + 50, (1 << 63) + 200, (1 << 64) - 1])
+def test_row_strides_beyond_the_address_space_are_refused(ld):
+    """Their byte ranges wrap around: without a check of their own they pass the one for overlaps."""
+    a, b, out, ws = _blocks(10, 200), _blocks(30, 200, 1 << 31, 1 << 41), 1 << 33, 1 << 42
+    pa, pb = ctypes.byref(a), ctypes.byref(b)
+    for status in (T.lib().cerar_quantize_blocks(1 << 20, 0, 10, 200, ld, 0, pa, None, None),
+                   T.lib().cerar_quantize_blocks(1 << 20, 1, 10, 200, ld, 1, pa, None, None),
+                   T.lib().cerar_matmul_blocks(pa, pb, out, 0, ld, 0, 0, ws, None),
+                   T.lib().cerar_linear_blocks(1 << 20, 1, 10, ld, pb, out, 0, 30, 0, ws, None),
+                   T.lib().cerar_linear_blocks(1 << 20, 1, 10, 200, pb, out, 1, ld, 0, ws, None)):
+        assert status == -1 and b"address space" in T.lib().cerar_last_error()
+
+
 def test_binding_refuses_host_tensors():
     x = torch.zeros(4, 4)
     for call in (lambda: T.GradSet([x]), lambda: T.TensorSet([x], [x]), lambda: T.quantize_blocks(x, rows=object()),
