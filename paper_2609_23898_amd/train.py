@@ -245,13 +245,20 @@ def grad_norm(tensors, clip, grad_scale=1.0, max_norm=math.inf, stream=None):
     C._check(lib().cerar_grad_norm(tensors.handle, grad_scale, max_norm, _clip(clip), _queue(stream, current)))
 
 
+def _settings(lr, beta1, beta2, eps, grad_scale, step, seed):
+    """cerar_adamw; a negative step would wrap to a large one (a seed may)."""
+    if step < 0:
+        raise ValueError(f"step={step}: the first step is 1")
+    return AdamWDesc(lr, beta1, beta2, eps, grad_scale, step, seed)
+
+
 def adamw_values(step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, seed=0):
     """What one step reads of its settings, as a uint8 host tensor: a program
     that replays a captured step copies the next one's into the device tensor
     that it gave as `values`."""
     import torch
     values = AdamWValues()
-    C._check(lib().cerar_adamw_pack(ctypes.byref(AdamWDesc(lr, beta1, beta2, eps, grad_scale, step, seed)),
+    C._check(lib().cerar_adamw_pack(ctypes.byref(_settings(lr, beta1, beta2, eps, grad_scale, step, seed)),
                                     ctypes.byref(values)))
     return torch.frombuffer(bytearray(values), dtype=torch.uint8)
 
@@ -273,7 +280,7 @@ def adamw_step(tensors, step=None, lr=None, beta1=0.9, beta2=0.999, eps=1e-8, gr
     else:
         if step is None or lr is None:
             raise ValueError("step and lr are needed")
-        hyper = ctypes.byref(AdamWDesc(lr, beta1, beta2, eps, grad_scale, step, seed))
+        hyper = ctypes.byref(_settings(lr, beta1, beta2, eps, grad_scale, step, seed))
     if clip is not None:
         current = C._on_device(clip, "clip", current)
         clip = _clip(clip)

@@ -131,6 +131,15 @@ def test_step_settings_beyond_fp32_are_refused(change):
     T.adamw_values(1, 1e-3, eps=2.0 ** -126)
 
 
+def test_negative_steps_are_refused():
+    """A negative number would wrap to one of some 2^64, whose bias corrections are 1."""
+    for step in (-1, -(1 << 63)):
+        with pytest.raises(ValueError, match="first step is 1"):
+            T.adamw_values(step, 1e-3)
+        with pytest.raises(ValueError, match="first step is 1"):
+            T.adamw_step(None, step, 1e-3)
+
+
 def test_step_values():
     v = T.AdamWValues.from_buffer_copy(bytes(T.adamw_values(3, 1e-2, 0.8, 0.99, 1e-6, 0.25, 5).numpy()))
     f = np.float32
