@@ -20,6 +20,7 @@ constexpr size_t scale_groups(size_t cols) { return (blocks_ld(cols) / kBlock + 
 
 // Threads of a launch along x: their count has 32 bits.
 constexpr uint64_t kMostThreads = 0xFFFFFFFFu;
+constexpr unsigned kComputeUnits = 256;              // of the card, which the variants' rules count on
 
 // Byte ranges of a call's buffers, for its overlap checks.
 inline bool ranges_meet(const void *a, size_t na, const void *b, size_t nb) {

@@ -524,7 +524,7 @@ inline Cut cut_of(size_t M, size_t N, size_t blocks, bool fast) {
     double least = 1e300;
     for (int R = 2; R <= 4; R += 2) {
         const double tiles = (double)((M + 64 * R - 1) / (64 * R)) * (double)((N + 64 * R - 1) / (64 * R));
-        const double block = fast ? (R == 4 ? 1.4 : 1.0) : (R == 4 ? 2.9 : 1.7), places = R == 4 ? 256 : 512;
+        const double block = fast ? (R == 4 ? 1.4 : 1.0) : (R == 4 ? 2.9 : 1.7), places = (R == 4 ? 1 : 2) * kComputeUnits;
         for (size_t parts = 1; parts <= 16; ++parts) {
             const size_t each = parts == 1 ? blocks : round_up((blocks + parts - 1) / parts, 4);
             if (parts > 1 && (parts - 1) * each >= blocks) continue;
@@ -552,7 +552,7 @@ void start(MatmulArgs g, int fa, int fb, bool fast, uint32_t parts, hipStream_t 
     const uint32_t tiles = g.tiles_m * g.tiles_n;
     // With fast sums a workgroup for each compute unit goes through the tiles; the
     // ring, two blocks long, is then never more than one tile ahead.
-    g.groups = fast && Lds<R>::kApart && g.blocks > 1 && parts == 1 ? std::min(tiles, 256u) : tiles;
+    g.groups = fast && Lds<R>::kApart && g.blocks > 1 && parts == 1 ? std::min(tiles, kComputeUnits) : tiles;
     hipLaunchKernelGGL(kernels[fa][fb][fast][g.bf16], dim3(g.groups, parts), dim3(256), Lds<R>::kBytes, stream, g);
 }
 

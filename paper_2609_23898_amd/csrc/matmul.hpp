@@ -24,7 +24,7 @@ constexpr size_t kFewRows = 64;
 // 9.5, 32 x 2048 x 512 7.1 and 7.2 against 6.4 and 9.5, 16 x 8192 x 512 9.8 against
 // 5.6 and 9.3.
 inline bool few_on_the_way(size_t M, size_t N, size_t ld) {
-    return N <= 16 * 256 ? M <= 32 && M * ld <= 12288 : M <= 8 && M * ld <= 8192;
+    return N <= 16 * kComputeUnits ? M <= 32 && M * ld <= 12288 : M <= 8 && M * ld <= 8192;
 }
 int matmul_few(const cerar_blocks &a, const cerar_blocks &b, void *out, cerar_type out_type, size_t ld_out, bool add,
                hipStream_t stream);

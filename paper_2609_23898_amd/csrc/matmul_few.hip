@@ -175,7 +175,7 @@ int start(FewArgs g, hipStream_t stream) {
     // once and two workgroups fit a compute unit (6.8 us, 12.3 with one), unless there are
     // fewer workgroups than compute units.
     constexpr bool kCodes = std::is_same_v<S, FromCodes>;
-    const unsigned groups = (g.N + 15) / 16, each = kCodes ? (MT == 1 ? 1 : 4) : groups >= 256 ? 4 : 1;
+    const unsigned groups = (g.N + 15) / 16, each = kCodes ? (MT == 1 ? 1 : 4) : groups >= kComputeUnits ? 4 : 1;
     g.waves = std::max(1u, std::min((g.blocks + each - 1) / each, kMostWaves));
     if (groups > kMostThreads / (64 * g.waves)) return fail(CERAR_E_INVAL, "a product too large for one launch");
     const size_t lds = g.waves * MT * 1024 + (kCodes ? 0 : (size_t)g.M * g.blocks * (kBlock + 1));

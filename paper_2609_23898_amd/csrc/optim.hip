@@ -24,7 +24,7 @@ constexpr int kPerThread = 4;                        // a block of 128 entries i
 constexpr int kSweep = kThreads * kPerThread;        // entries that a workgroup takes at a time
 constexpr unsigned kPieceShift = 3;                   // of a piece's sweeps at most
 constexpr int kPlaces = 2048;                        // workgroups that the card holds at a time, about
-constexpr int kNormGroups = 512;                    // workgroups of the norm at most: two on each compute unit
+constexpr int kNormGroups = 2 * kComputeUnits;       // workgroups of the norm at most
 
 struct Piece {
     uint32_t tensor, sweeps;
