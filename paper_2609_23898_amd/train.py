@@ -205,7 +205,8 @@ class TensorSet(_Set):
         def length(name, n):
             return -(-n // BLOCK) if name.endswith("scale") else n
 
-        if states is None:
+        made = states is None
+        if made:
             states = {name: [torch.zeros(length(name, p.numel()), dtype=dt, device=p.device) for p in params]
                       for name, dt in kinds.items()}
         if set(states) != set(kinds) or any(len(states[name]) != count for name in kinds):
@@ -228,6 +229,8 @@ class TensorSet(_Set):
         counted = {id(t if t._base is None else t._base): t for t in params + list(copies or [])}
         self._stepped = list(counted.values())
         self._create(descs, state_bits, (params, grads, copies, states))
+        if made:
+            torch.cuda.current_stream().synchronize()    # they are zero before a step on any stream
 
 
 def _clip(clip):

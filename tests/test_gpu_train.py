@@ -1053,6 +1053,22 @@ def test_step_on_another_stream():
         assert torch.equal(u, v)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_states_made_on_a_busy_stream_are_zero_before_a_step_on_another(bits):
+    torch, dev = torch_dev()
+    busy, other = torch.cuda.Stream(), torch.cuda.Stream()
+    p, g = torch.ones(5000, device=dev), torch.ones(5000, device=dev)
+    x, y = torch.ones((4096, 4096), device=dev), torch.empty((4096, 4096), device=dev)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(busy):
+        for _ in range(40):
+            torch.mm(x, x, out=y)
+        s = T.TensorSet([p], [g], state_bits=bits)
+    T.adamw_step(s, 1, 1e-3, stream=other)
+    torch.cuda.synchronize()
+    assert bool((s.states["m"][0].float() != 0).all()) and bool((s.states["v"][0].float() != 0).all())
+
+
 def test_values_equal_the_settings():
     torch, dev = torch_dev()
     out = []
