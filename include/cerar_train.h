@@ -150,7 +150,8 @@ int cerar_quantize_blocks(const void *x, cerar_type type, size_t rows, size_t co
                           const cerar_blocks *by_row, const cerar_blocks *by_col, cerar_stream stream);
 
 /* Device workspace of cerar_matmul_blocks (linear = 0) or cerar_linear_blocks
- * (linear = 1) for out (M x N) and inner length K; may be 0.  Errors: E_INVAL
+ * (linear = 1) for out (M x N) and inner length K; may be 0.  A linear call asks for
+ * room for its quantised activations also where few rows leave it alone.  Errors: E_INVAL
  * (NULL; M or N of 2^31 or more, K of 2^23 or more). */
 int cerar_matmul_workspace_bytes(size_t M, size_t N, size_t K, int linear, size_t *bytes);
 
@@ -162,8 +163,7 @@ int cerar_matmul_workspace_bytes(size_t M, size_t N, size_t K, int linear, size_
  * them and keep 13 bits below its leading one: a relative error of 1.5e-5 of
  * the result for normally distributed codes (5e-5 where their magnitudes span
  * the whole format), which matters to an fp32 result and not to a bf16 one.
- * Products of 64 rows of A or fewer, which the reading of B bounds, are summed
- * in fp32 either way. */
+ * Products of 64 rows of A or fewer are summed in fp32 either way. */
 typedef enum { CERAR_SUMS_F32 = 0, CERAR_SUMS_FAST = 1 } cerar_sums;
 
 /* out (device, M x N of out_type, row stride ld_out entries) = A B^T, or with

@@ -12,8 +12,11 @@ int quantize(const void *x, cerar_type type, size_t rows, size_t cols, size_t ld
              const cerar_blocks *by_row, const cerar_blocks *by_col, hipStream_t stream);
 
 // Products of few rows (matmul_few.hip): out = A B^T, or out and that, for A in the
-// block format with at most kFewRows rows.  At 45 x 6145 x 2050 few rows take 14.6 us
-// and a tile of 128 x 128 over parts of K 17, at 100 rows the tile 20 and this 23.
+// block format with at most kFewRows rows.  Against tiles of 128 x 128 over parts of K,
+// fp32 sums, us a call: 64 x 2048 x 512 5.7 and 9.2, 64 x 8192 x 2048 12.5 and 17.0, 64 x 6145 x
+// 2050 13.2 and 17.3; 100 x 6145 x 2050 23 and 20.  Long rows of many columns are better off
+// in tiles before that: 64 x 2048 x 8192 21.6 and 20.3, 16 x 16384 x 8192 36.1 and 40.6, 32 of them
+// 54 and 40, 64 of them 87 and 44.
 constexpr size_t kFewRows = 64;
 
 // Whether M x ld activations (ld: K rounded up) are quantised on the way, by each of

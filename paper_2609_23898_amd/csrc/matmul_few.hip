@@ -1,7 +1,9 @@
 // Products of few rows in the 8-bit block format: out = A B^T for the tokens that a
 // model answers with, one or a few dozen at a time.
 //
-// The bound is reading B once.  A workgroup takes 16 rows of B; its waves share out
+// The floor is reading B once.  Up to 16 rows of A come within a few microseconds of it
+// (8192 x 2048 6.7 us a call, 16384 x 8192 36); with more, widening codes bounds them: 45 x 6145 x
+// 2050 takes 12.3 us on the device, its B 1.9.  A workgroup takes 16 rows of B; its waves share out
 // the blocks along K and add their results in LDS, in the waves' order.  A lane
 // loads 32 bytes of one row of B for a block, four blocks at a time, straight into
 // registers: with the loads of all waves in flight before the first product, K is
@@ -10,8 +12,8 @@
 // rounding; the block's scales are added to the sum's exponent.
 //
 // Activations are quantised into LDS by the workgroups that multiply with them, while
-// their first loads of B are on their way, so that a layer is one launch with no
-// workspace.
+// their first loads of B are on their way, so that a layer is one launch that
+// leaves its workspace alone.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
